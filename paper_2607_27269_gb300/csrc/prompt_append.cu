@@ -71,6 +71,10 @@ __global__ void __launch_bounds__(kThreads) prompt_append_kernel(const __grid_co
     const int t0 = blockIdx.x * nt, n = min(nt, p.total - t0);
     // (writes caches: no early trigger, see append.cu)
     griddep_wait();
+    if (blockIdx.x == 0) {
+        for (int b = tid; b < p.batch; b += kThreads)
+            if (p.cu[b] < 0 || p.cu[b + 1] < p.cu[b] || p.cu[b + 1] > p.total) record_status(p.status, kStatusBounds);
+    }
     if (warp < n) {
         // the sequence: as many as end at or before the token
         const int t = t0 + warp;
@@ -81,11 +85,13 @@ __global__ void __launch_bounds__(kThreads) prompt_append_kernel(const __grid_co
             int pos = kNone;
             if (before < p.batch) {
                 const int first = p.cu[before], end = p.cu[before + 1];
-                if (first >= 0 && first <= t && end <= p.total) {
+                if (first >= 0 && first <= t && end <= p.total) {  // (else the token is no sequence's)
                     const int64_t at = static_cast<int64_t>(p.start[before]) + (t - first);
-                    if (at >= 0 && at < INT32_MAX) pos = static_cast<int>(at);
+                    if (at >= 0 && at < INT32_MAX)
+                        pos = static_cast<int>(at);
+                    else
+                        record_status(p.status, kStatusBounds);
                 }
-                if (pos == kNone) record_status(p.status, kStatusBounds);
             }
             s_pos[warp] = pos;
             s_seq[warp] = before;
