@@ -319,7 +319,9 @@ mla_status mla_gqa_out_proj(const mla_gqa_dims *dims, int32_t batch, int32_t q_l
  * stride between tokens (in elements, a multiple of 8, at least heads *
  * head_dim), so that the three may be parts of one projection's output.
  * Bases are 16-byte aligned.  A sequence whose offsets fall, are negative or
- * pass `total` is skipped and recorded as MLA_ERR_DEVICE_BOUNDS.  Tokens that
+ * pass `total` is skipped and recorded as MLA_ERR_DEVICE_BOUNDS; the others are
+ * served (where offsets fall two of them may claim a token: appending, the first
+ * has it).  Tokens that
  * belong to no sequence (before cu_seqlens[0], past the last sequence) are left
  * alone and are no fault. */
 

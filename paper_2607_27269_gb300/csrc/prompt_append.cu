@@ -76,25 +76,25 @@ __global__ void __launch_bounds__(kThreads) prompt_append_kernel(const __grid_co
             if (p.cu[b] < 0 || p.cu[b + 1] < p.cu[b] || p.cu[b + 1] > p.total) record_status(p.status, kStatusBounds);
     }
     if (warp < n) {
-        // the sequence: as many as end at or before the token
+        // the first sequence that holds the token, if any does (others' offsets may fall)
         const int t = t0 + warp;
-        int before = 0;
-        for (int b = lane; b < p.batch; b += 32) before += p.cu[b + 1] <= t;
-        before = __reduce_add_sync(0xffffffffu, before);
+        int seq = INT32_MAX;
+        for (int b = lane; b < p.batch; b += 32) {
+            const int first = p.cu[b], end = p.cu[b + 1];
+            if (first >= 0 && first <= t && t < end && end <= p.total) seq = min(seq, b);
+        }
+        seq = __reduce_min_sync(0xffffffffu, seq);
         if (lane == 0) {
             int pos = kNone;
-            if (before < p.batch) {
-                const int first = p.cu[before], end = p.cu[before + 1];
-                if (first >= 0 && first <= t && end <= p.total) {  // (else the token is no sequence's)
-                    const int64_t at = static_cast<int64_t>(p.start[before]) + (t - first);
-                    if (at >= 0 && at < INT32_MAX)
-                        pos = static_cast<int>(at);
-                    else
-                        record_status(p.status, kStatusBounds);
-                }
+            if (seq != INT32_MAX) {
+                const int64_t at = static_cast<int64_t>(p.start[seq]) + (t - p.cu[seq]);
+                if (at >= 0 && at < INT32_MAX)
+                    pos = static_cast<int>(at);
+                else
+                    record_status(p.status, kStatusBounds);
             }
             s_pos[warp] = pos;
-            s_seq[warp] = before;
+            s_seq[warp] = seq;
         }
     }
     __syncthreads();

@@ -63,3 +63,25 @@ def test_append_tokens_of_no_sequence(cu, total, owned):
 ])
 def test_append_records_faulty_offsets(cu, total, owned):
     check_owners(cu, total, abi.MLA_ERR_DEVICE_BOUNDS, owned)
+
+
+@pytest.mark.parametrize("cu,total,owned", [
+    ([0, 50, 40, 110], 110, [(0, 0, 0, 50), (2, 10, 50, 110)]),
+    ([0, 20, 10, 15, 30], 30, [(0, 0, 0, 20), (3, 5, 20, 30)]),
+    ([0, 10, 10, 7], 10, [(0, 0, 0, 10)]),
+    ([30, 20, 30, 5, 5], 40, [(1, 0, 20, 30)]),
+    ([0, 10, 90, 15, 30], 30, [(0, 0, 0, 10), (3, 0, 15, 30)]),
+])
+def test_append_serves_sound_sequences_beside_faulty_ones(cu, total, owned):
+    """A sequence whose own offsets are sound has all its tokens written, wherever others' fall; of two that claim a
+    token the first has it."""
+    check_owners(cu, total, abi.MLA_ERR_DEVICE_BOUNDS, owned)
+
+
+def test_append_finds_sequences_far_down():
+    """More sequences than a warp has lanes, empty ones among them, faulty ones too."""
+    n = [(i * 5) % 4 for i in range(100)]
+    cu = [0] + np.cumsum(n).tolist()
+    check_owners(cu, cu[-1], abi.MLA_OK, [(b, 0, cu[b], cu[b + 1]) for b in range(100)], G=1)
+    cu[70] = 1 << 30  # the 69th ends and the 70th begins past the tokens
+    check_owners(cu, cu[-1], abi.MLA_ERR_DEVICE_BOUNDS, [(b, 0, cu[b], cu[b + 1]) for b in range(100) if b not in (69, 70)], G=1)
