@@ -360,7 +360,8 @@ mla_status mla_gqa_prompt_workspace_size(const mla_gqa_dims *dims, int32_t batch
  * A query at a negative position (n_b > kv_len[b]) sees no key: o = 0, lse =
  * -inf.  Rows of q_rot, o and lse that belong to no sequence are left alone.
  * Key and value rows at kv_len[b] and beyond may hold anything; rows below it
- * are finite.  kv_len[b] outside [0, max_kv_len] is recorded and counts as 0.
+ * are finite.  A query that is not finite makes its own o and lse NaN (lse -inf
+ * where all its scores are) and no others.  kv_len[b] outside [0, max_kv_len] is recorded and counts as 0.
  *   q_rot [total, H, head_dim] bf16 (rotated, token stride q_stride), kv_len
  *   [batch] int32 device, o [total, H, head_dim] bf16, lse [total, H] fp32 or
  *   NULL; o_part / lse_part sized by mla_gqa_prompt_workspace_size (NULL where

@@ -91,7 +91,7 @@ struct Args {
 // partition with a piece of it, -1 where none begins here), and whether its own
 // first piece goes on with another partition's item.
 struct Cut {
-    int tok, ntok, g, last, goes_on, pad[3];
+    int tok, ntok, pos, g, last, goes_on, pad[2];
 };
 
 // What the warps work on next: an item's key tiles [t0, t0 + n), n the larger of
@@ -494,10 +494,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             const List list = locate(a, part, at, end);
             if (a.cut && lane == 0) {
                 // (T > 0 where an end lies in an item)
-                Cut c{0, 0, 0, -1, at.t > 0 && !(at.same(end) && at.t >= end.t), {}};
+                Cut c{0, 0, 0, 0, -1, at.t > 0 && !(at.same(end) && at.t >= end.t), {}};
                 if (end.b < a.batch && end.t > 0 && !(at.same(end) && at.t > 0)) {
                     c.tok = a.cu[end.b] + end.k * per;
                     c.ntok = min(per, end.s.n - end.k * per);
+                    c.pos = end.s.p0 + end.k * per;
                     c.g = end.g;
                     c.last = list.part_of(a, end.at + a.item + static_cast<int64_t>(tiles_of(end.s, per, end.k) - list.least + 1) * kTile - 1);
                 }
@@ -871,8 +872,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             // ---- the rows
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            const float lse = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            // A row of an item's piece may see none of its keys, one of a whole item sees
+            // none before position 0: 0.  What else has no sum, or NaN for one, shows.
+            const bool none = l == 0.f && (slot >= 0 || pos < 0);
+            const float inv = none ? 0.f : 1.f / l;
+            const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
             const int64_t at = (t * a.groups + g) * a.hpg + hh;
             const int part_row = (slot * 2 + h) * kTile;
             if (real && slot >= 0) a.lse_part[part_row + row] = lse;
@@ -1028,12 +1032,12 @@ __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const __grid_
         }
     }
     const int64_t at = (static_cast<int64_t>(cut.tok + in) * a.groups + cut.g) * a.hpg + row % a.hpg;
-    const float inv = w > 0.f ? 1.f / w : 0.f;
+    const float inv = w == 0.f && cut.pos + in < 0 ? 0.f : 1.f / w;  // (no key before position 0)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         *reinterpret_cast<uint2 *>(a.o + at * D + c + 4 * TPR * i) =
             make_uint2(pack_bf16(acc[4 * i] * inv, acc[4 * i + 1] * inv), pack_bf16(acc[4 * i + 2] * inv, acc[4 * i + 3] * inv));
-    if (a.lse && c == 0) a.lse[at] = w > 0.f ? m + log2f(w) * 0.69314718055994531f : -INFINITY;
+    if (a.lse && c == 0) a.lse[at] = w == 0.f ? -INFINITY : m + log2f(w) * 0.69314718055994531f;
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder()

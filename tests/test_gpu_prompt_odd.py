@@ -85,3 +85,59 @@ def test_append_finds_sequences_far_down():
     check_owners(cu, cu[-1], abi.MLA_OK, [(b, 0, cu[b], cu[b + 1]) for b in range(100)], G=1)
     cu[70] = 1 << 30  # the 69th ends and the 70th begins past the tokens
     check_owners(cu, cu[-1], abi.MLA_ERR_DEVICE_BOUNDS, [(b, 0, cu[b], cu[b + 1]) for b in range(100) if b not in (69, 70)], G=1)
+
+
+@pytest.mark.parametrize("splits", [0, 1, 5, 40])
+@pytest.mark.parametrize("H,G,d", [(14, 2, 64), (8, 2, 128)])
+def test_queries_that_are_not_finite_show(H, G, d, splits):
+    """NaN and infinities in a query reach its row of o and lse, whole items and cut ones alike, and no other row.  A row
+    all of whose scores are -inf has the log-sum-exp -inf of the formula, and weights of 0 / 0."""
+    n, kv = [40, 150, 30], [6000, 150, 300]
+    L = Layer(H, G, d, kv, True, seed=32)
+    for b in range(3):
+        for g in range(G):
+            at = L.at(b, g, kv[b])
+            L.k[at[0], at[1], 2] = L.k[at[0], at[1], 2].abs() + 1  # (one sign: a score's infinity has the query's)
+    q = L.normal(220, H, d)
+
+    def run(x):
+        step = abi.GqaPrompt(L.dims, L.cache, 3, 220, 6000, splits)
+        return step.attend(x, cu_of(n), i32(kv)).clone(), step.lse.clone()
+
+    o, lse = run(q)
+    bad = q.clone()
+    bad[17, 3, 9] = math.nan
+    bad[18] = math.nan
+    bad[20, 1, 2] = math.inf        # every score +inf
+    bad[25, 5, 5] = math.inf        # scores of both infinities
+    bad[60, 0] = math.inf           # infinities of both signs add to NaN
+    bad[189, H - 1, 0] = math.nan   # the last token of its sequence
+    bad[200, 2, 1] = -math.inf
+    only = bad.clone()
+    only[30, 4, 2] = -math.inf      # every score -inf
+    only[100, 6, 2] = -math.inf
+    o2, lse2 = run(only)
+    assert abi.check_status() == abi.MLA_OK
+    hit = torch.zeros(220, H, dtype=torch.bool, device="cuda")
+    for t, h in ((17, 3), (18, slice(None)), (20, 1), (25, 5), (60, 0), (189, H - 1), (200, 2)):
+        hit[t, h] = True
+    dark = torch.zeros_like(hit)
+    dark[30, 4] = dark[100, 6] = True
+    assert torch.isnan(lse2[hit]).all() and torch.isneginf(lse2[dark]).all()
+    assert torch.isnan(o2[hit | dark].float()).all()
+    rest = ~(hit | dark)
+    assert torch.equal(o2[rest], o[rest]) and torch.equal(lse2[rest], lse[rest])
+
+
+def test_rows_without_keys_stay_empty():
+    """Queries at negative positions see no key whatever they hold: o = 0, lse = -inf, in whole items and cut ones."""
+    n, kv = [90, 700], [30, 4000]
+    L = Layer(8, 2, 64, kv, False, seed=33)
+    q = L.normal(790, 8, 64)
+    q[:60] = math.nan
+    for splits in (0, 1, 30):
+        step = abi.GqaPrompt(L.dims, L.cache, 2, 790, 4000, splits)
+        o = step.attend(q, cu_of(n), i32(kv))
+        assert abi.check_status() == abi.MLA_OK
+        assert (o[:60] == 0).all() and torch.isneginf(step.lse[:60]).all()
+        assert torch.isfinite(o[60:].float()).all() and torch.isfinite(step.lse[60:]).all()
