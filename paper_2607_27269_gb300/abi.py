@@ -337,6 +337,14 @@ def _i32(t: Optional[torch.Tensor]):
     return _p(t)
 
 
+def _room(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, device: torch.device):
+    """A caller's tensor holds what a call writes: rows of `width` entries, one behind the other."""
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"outputs must be {dtype} tensors on {device}")
+    if t.numel() < rows * width or (t.dim() > 1 and t.shape[-1] != width) or not t.is_contiguous():
+        raise ValueError(f"outputs must be contiguous and hold {rows} rows of {width}")
+
+
 def gqa_prompt_workspace_size(dims: GqaDims, batch: int, total: int, max_kv_len: int, num_splits: int = 0):
     """(o_part_bytes, lse_part_bytes, num_splits_used)."""
     ob, lb, s = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_int32()
@@ -441,15 +449,20 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], n_top: 
                    lse: Optional[torch.Tensor] = None, stream=None):
     """logits [rows, vocab] (fp32 or bf16, any row stride) -> the log probability of each row's token (int32; None: not
     asked for), the entropy, and the indices and log probabilities of the n_top likeliest tokens, written into the given
-    device tensors (allocated if None; ``lse`` only if given)."""
+    device tensors (fp32 but for the int32 indices, of rows entries or rows x n_top at least; allocated if None; ``lse``
+    only if given)."""
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda:
         raise ValueError("logits must be a 2-d fp32 or bf16 CUDA tensor")
     rows, vocab = logits.shape
     if logits.stride(1) != 1 and vocab > 1:
         raise ValueError("logits must have unit inner stride")
-    if tokens is not None and tokens.shape[0] != rows:
-        raise ValueError("tokens holds one entry per row")
     dev = logits.device
+    if tokens is not None and (tokens.shape[0] != rows or tokens.device != dev):
+        raise ValueError("tokens holds one entry per row, on the logits' device")
+    for t, width, dtype in ((logprob, 1, torch.float32), (entropy, 1, torch.float32), (lse, 1, torch.float32),
+                            (top_index, n_top, torch.int32), (top_logprob, n_top, torch.float32)):
+        if t is not None and width:
+            _room(t, rows, width, dtype, dev)
     if logprob is None and tokens is not None:
         logprob = torch.empty(rows, dtype=torch.float32, device=dev)
     entropy = torch.empty(rows, dtype=torch.float32, device=dev) if entropy is None else entropy

@@ -1,0 +1,122 @@
+"""The binding's own checks of prompt, score and page calls, on stand-ins for device tensors (nothing is launched)."""
+from __future__ import annotations
+
+import contextlib
+import weakref
+
+import pytest
+import torch
+
+from paper_2607_27269_gb300 import abi
+
+F32, BF16, F16, I32, I64 = torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64
+GPU = torch.device("cuda", 0)
+
+
+class Fake:
+    """What the binding asks of a tensor on a GPU."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=F32, device=GPU, strides=None, stream=None):
+        self.shape, self.dtype, self.device, self.stream = torch.Size(shape), dtype, device, stream
+        dense = [1]
+        for n in reversed(shape[1:]):
+            dense.insert(0, dense[0] * n)
+        self._strides = tuple(dense[:len(shape)]) if strides is None else strides
+        self._dense = strides is None
+
+    def stride(self, i=None):
+        return self._strides if i is None else self._strides[i]
+
+    def size(self, i):
+        return self.shape[i]
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return self._dense
+
+    def data_ptr(self):
+        return 0x10000
+
+    def __getitem__(self, at):
+        return Fake(len(range(*at.indices(self.shape[0]))), *self.shape[1:], dtype=self.dtype, device=self.device,
+                    stream=self.stream)
+
+
+class Calls:
+    """The library: every call is noted and succeeds."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.made.append((name, args))
+            return abi.MLA_OK
+        return call
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls; torch.empty makes stand-ins that know the stream on which they were allocated."""
+    made, on = Calls(), ["current"]
+
+    @contextlib.contextmanager
+    def stream_of(s):
+        on.append(s)
+        yield
+        on.pop()
+
+    def empty(*shape, dtype=None, device=None):
+        return Fake(*(shape[0] if len(shape) == 1 and not isinstance(shape[0], int) else shape), dtype=dtype,
+                    device=torch.device(device), stream=on[-1])
+
+    monkeypatch.setattr(abi, "lib", lambda: made)
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "stream", stream_of)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, **kw: ("external", handle))
+    monkeypatch.setattr(abi, "_stream", lambda s: 0 if s is None else s if isinstance(s, int) else s.cuda_stream)
+    return made
+
+
+@pytest.mark.parametrize("name,bad", [
+    (name, bad) for name in ("logprob", "entropy", "lse")
+    for bad in (Fake(3, dtype=BF16), Fake(3, dtype=F16), Fake(3, dtype=torch.float64), Fake(2), Fake(0), Fake(1),
+                Fake(3, device=torch.device("cuda", 1)), Fake(3, 2))
+] + [("top_index", bad) for bad in (Fake(3, 4, dtype=I32), Fake(2, 5, dtype=I32), Fake(14, dtype=I32), Fake(3, 5, dtype=I64),
+                                    Fake(3, 5), Fake(5, 3, dtype=I32), Fake(3, 5, dtype=I32, strides=(8, 1)))]
+  + [("top_logprob", bad) for bad in (Fake(3, 4), Fake(2, 5), Fake(3, 5, dtype=BF16), Fake(3, 6), Fake(3))])
+def test_score_outputs_that_do_not_fit_are_refused(calls, name, bad):
+    x, tokens = Fake(3, 100), Fake(3, dtype=I32)
+    good = dict(logprob=Fake(3), entropy=Fake(3), lse=Fake(3), top_index=Fake(3, 5, dtype=I32), top_logprob=Fake(3, 5))
+    abi.token_logprobs(x, tokens, 5, **good)
+    assert len(calls.made) == 1
+    with pytest.raises(ValueError):
+        abi.token_logprobs(x, tokens, 5, **{**good, name: bad})
+    assert len(calls.made) == 1  # (nothing was called)
+
+
+def test_score_inputs_that_do_not_fit_are_refused(calls):
+    for tokens in (Fake(2, dtype=I32), Fake(3, dtype=I64), Fake(3, dtype=I32, strides=(2,)),
+                   Fake(3, dtype=I32, device=torch.device("cuda", 1))):
+        with pytest.raises(ValueError):
+            abi.token_logprobs(Fake(3, 100), tokens, 0)
+    assert not calls.made
+
+
+def test_score_outputs_with_room_to_spare_are_taken(calls):
+    out = abi.token_logprobs(Fake(3, 100), Fake(3, dtype=I32), 5, Fake(4), Fake(3, 1), Fake(9, 5, dtype=I32), Fake(15))
+    assert len(calls.made) == 1 and [t.numel() for t in out] == [4, 3, 45, 15]
+    assert abi.token_logprobs(Fake(3, 100), None, 0, top_index=Fake(1, dtype=I32))[2].numel() == 1  # (not written)
+
+
+def test_score_results_are_made_where_none_are_given(calls):
+    out = abi.token_logprobs(Fake(3, 100, dtype=BF16), Fake(3, dtype=I32), 4)
+    assert [tuple(t.shape) for t in out] == [(3,), (3,), (3, 4), (3, 4)]
+    assert [t.dtype for t in out] == [F32, F32, I32, F32]
+    assert abi.token_logprobs(Fake(3, 100), None)[0] is None
