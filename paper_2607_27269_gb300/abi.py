@@ -7,6 +7,7 @@ library's kernels.  PyTorch supplies device memory and streams.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import threading
@@ -155,6 +156,17 @@ def _stream(stream) -> Optional[int]:
             return _raw_stream(_raw_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_here = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """Where what a call writes on ``stream`` is allocated: in that stream's memory, since a block of the current
+    stream's may still be in use by work queued there, and is handed out again there when its tensor goes."""
+    if stream is None:
+        return _here
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -463,11 +475,12 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], n_top: 
                             (top_index, n_top, torch.int32), (top_logprob, n_top, torch.float32)):
         if t is not None and width:
             _room(t, rows, width, dtype, dev)
-    if logprob is None and tokens is not None:
-        logprob = torch.empty(rows, dtype=torch.float32, device=dev)
-    entropy = torch.empty(rows, dtype=torch.float32, device=dev) if entropy is None else entropy
-    top_index = torch.empty(rows, n_top, dtype=torch.int32, device=dev) if top_index is None else top_index
-    top_logprob = torch.empty(rows, n_top, dtype=torch.float32, device=dev) if top_logprob is None else top_logprob
+    with _memory_of(stream):
+        if logprob is None and tokens is not None:
+            logprob = torch.empty(rows, dtype=torch.float32, device=dev)
+        entropy = torch.empty(rows, dtype=torch.float32, device=dev) if entropy is None else entropy
+        top_index = torch.empty(rows, n_top, dtype=torch.int32, device=dev) if top_index is None else top_index
+        top_logprob = torch.empty(rows, n_top, dtype=torch.float32, device=dev) if top_logprob is None else top_logprob
     _check("mla_token_logprobs", lib().mla_token_logprobs(
         rows, vocab, 0 if logits.dtype == torch.float32 else 1, logits.data_ptr(),
         logits.stride(0) if rows > 1 else vocab, _i32(tokens), n_top, _p(logprob), _p(entropy), _p(lse), _i32(top_index),
@@ -537,7 +550,9 @@ def e2e_loss(a_mla: torch.Tensor, a_orig: torch.Tensor, mask: Optional[torch.Ten
     post-W_O outputs, bf16 [.., D]); returns a one-element fp32 device tensor."""
     hidden = a_mla.shape[-1]
     rows = a_mla.numel() // hidden
-    loss = torch.empty(1, dtype=torch.float32, device=a_mla.device) if loss is None else loss
+    if loss is None:
+        with _memory_of(stream):
+            loss = torch.empty(1, dtype=torch.float32, device=a_mla.device)
     _check("mla_e2e_loss", lib().mla_e2e_loss(rows, hidden, _p(a_mla), _p(a_orig), _p(mask), _p(loss),
                                               _stream(stream)))
     return loss
@@ -588,10 +603,11 @@ def acceptance_stats(draft: torch.Tensor, target: torch.Tensor, alpha: Optional[
         raise ValueError("logits must be CUDA tensors with unit inner stride and equal row strides")
     row_stride = draft.stride(0) if rows > 1 else vocab
     dev = draft.device
-    alpha = torch.empty(rows, dtype=torch.float32, device=dev) if alpha is None else alpha
-    argmax_draft = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_draft is None else argmax_draft
-    argmax_target = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_target is None else argmax_target
-    greedy = torch.empty(rows, dtype=torch.int32, device=dev) if greedy is None else greedy
+    with _memory_of(stream):
+        alpha = torch.empty(rows, dtype=torch.float32, device=dev) if alpha is None else alpha
+        argmax_draft = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_draft is None else argmax_draft
+        argmax_target = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_target is None else argmax_target
+        greedy = torch.empty(rows, dtype=torch.int32, device=dev) if greedy is None else greedy
     _check("mla_acceptance_stats", lib().mla_acceptance_stats(rows, vocab, 0 if draft.dtype == torch.float32 else 1,
                                                               draft.data_ptr(), target.data_ptr(), row_stride,
                                                               _p(alpha),

@@ -120,3 +120,21 @@ def test_score_results_are_made_where_none_are_given(calls):
     assert [tuple(t.shape) for t in out] == [(3,), (3,), (3, 4), (3, 4)]
     assert [t.dtype for t in out] == [F32, F32, I32, F32]
     assert abi.token_logprobs(Fake(3, 100), None)[0] is None
+
+
+class Stream:
+    cuda_stream = 77
+
+
+@pytest.mark.parametrize("stream", [None, Stream(), 77])
+def test_results_are_allocated_on_the_stream_that_writes_them(calls, monkeypatch, stream):
+    """Memory of the current stream may still be in use by work queued there: what a call on another stream writes comes
+    from that stream's memory."""
+    want = "current" if stream is None else stream if isinstance(stream, Stream) else ("external", 77)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    x, rows = Fake(3, 100), Fake(3, 64, dtype=BF16)
+    made = [*abi.token_logprobs(x, Fake(3, dtype=I32), 4, stream=stream), *abi.acceptance_stats(x, x, stream=stream),
+            abi.e2e_loss(rows, rows, stream=stream)]
+    assert len(made) == 9 and all(t.stream == want for t in made)
+    given = abi.token_logprobs(x, None, 0, entropy=(e := Fake(3)), stream=stream)
+    assert given[1] is e
