@@ -369,7 +369,9 @@ def gqa_prompt_workspace_size(dims: GqaDims, batch: int, total: int, max_kv_len:
 class GqaPrompt:
     """Whole prompts of an original GQA layer: packed ragged sequences of up to
     ``batch`` sequences and ``max_tokens`` tokens a call, with every buffer
-    allocated once.  ``append`` writes a call's keys and values to the cache and
+    allocated once (the rotated queries', the projections' and each hidden
+    width's at their first use, in the memory of that call's stream) and kept as
+    long as the handle, which has to outlive the work queued with it.  ``append`` writes a call's keys and values to the cache and
     rotates its queries, ``attend`` runs the causal attention over the cache
     (o [total, H, head_dim] bf16, ``lse`` [total, H]), ``__call__`` both, and
     ``from_hidden`` the whole layer from hidden states to its output
@@ -386,7 +388,8 @@ class GqaPrompt:
         self._parts = _p(self._o_part), _p(self._lse_part)
         self._o = torch.empty(max_tokens, H, d, dtype=torch.bfloat16, device=dev)
         self._lse = torch.empty(max_tokens, H, dtype=torch.float32, device=dev)
-        self._q = None
+        self._q = self._proj = None
+        self._outs = {}  # of from_hidden, by hidden width
         self._views = 0, self._o[:0], self._lse[:0]  # of the last call's length
         self.lse = self._views[2]
         # the layer's descriptors are fixed: marshalled once
@@ -408,7 +411,8 @@ class GqaPrompt:
         H, G, w = d.num_heads, d.num_kv_groups, d.head_dim
         if q is not None and q_rot is None:
             if self._q is None:
-                self._q = torch.empty(self.max_tokens, H, w, dtype=torch.bfloat16, device=k.device)
+                with _memory_of(stream):
+                    self._q = torch.empty(self.max_tokens, H, w, dtype=torch.bfloat16, device=k.device)
             q_rot = self._q[:total]
         _check("mla_gqa_prompt_append", lib().mla_gqa_prompt_append(
             *self._refs, batch, total, _i32(cu_seqlens), _i32(start_pos), *_rows(q, H, w, total),
@@ -438,14 +442,16 @@ class GqaPrompt:
         out [total, hidden] bf16."""
         d, (total, hidden) = self.dims, h.shape
         self._sizes(total, kv_len.shape[0])
-        if getattr(self, "_proj", None) is None or self._out.shape[1] != hidden:
+        with _memory_of(stream):
             new = lambda *s: torch.empty(self.max_tokens, *s, dtype=torch.bfloat16, device=h.device)
-            self._proj = (new(d.num_heads, d.head_dim), *(new(d.num_kv_groups, d.head_dim) for _ in range(2)))
-            self._out = new(hidden)
+            if self._proj is None:
+                self._proj = (new(d.num_heads, d.head_dim), *(new(d.num_kv_groups, d.head_dim) for _ in range(2)))
+            if hidden not in self._outs:
+                self._outs[hidden] = new(hidden)
         q, k, v = (t[:total] for t in self._proj)
         gqa_project(d, h[None], w_q, w_k, w_v, q, k, v, stream)
         o = self.attend(self.append(q, k, v, cu_seqlens, start_pos, q, stream), cu_seqlens, kv_len, stream)
-        return gqa_prompt_out_proj(d, o, w_o, self._out[:total], stream)
+        return gqa_prompt_out_proj(d, o, w_o, self._outs[hidden][:total], stream)
 
 
 def gqa_prompt_out_proj(dims: GqaDims, o: torch.Tensor, w_o: torch.Tensor, out: torch.Tensor, stream=None):

@@ -44,8 +44,8 @@ class Fake:
         return 0x10000
 
     def __getitem__(self, at):
-        return Fake(len(range(*at.indices(self.shape[0]))), *self.shape[1:], dtype=self.dtype, device=self.device,
-                    stream=self.stream)
+        shape = (1, *self.shape) if at is None else (len(range(*at.indices(self.shape[0]))), *self.shape[1:])
+        return Fake(*shape, dtype=self.dtype, device=self.device, stream=self.stream)
 
 
 class Calls:
@@ -138,3 +138,43 @@ def test_results_are_allocated_on_the_stream_that_writes_them(calls, monkeypatch
     assert len(made) == 9 and all(t.stream == want for t in made)
     given = abi.token_logprobs(x, None, 0, entropy=(e := Fake(3)), stream=stream)
     assert given[1] is e
+
+
+def handle(monkeypatch, max_tokens=10):
+    monkeypatch.setattr(abi, "gqa_prompt_workspace_size", lambda *a: (0, 0, 1))
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    dims = abi.GqaDims(4, 2, 64, 0.125)
+    cache = abi.Cache(Fake(4, 64, 64, dtype=BF16), Fake(4, 64, 64, dtype=BF16), 64)
+    return abi.GqaPrompt(dims, cache, 2, max_tokens, 64)
+
+
+def test_prompt_buffers_are_allocated_on_the_stream_that_writes_them(calls, monkeypatch):
+    """Buffers that a handle makes at their first use, too."""
+    h, side = handle(monkeypatch), Stream()
+    cu, pos = Fake(3, dtype=I32), Fake(2, dtype=I32)
+    rot = h.append(Fake(7, 4, 64, dtype=BF16), *(Fake(7, 2, 64, dtype=BF16) for _ in range(2)), cu, pos, stream=side)
+    assert rot.stream is side
+    w = [Fake(n * 64, 96, dtype=BF16) for n in (4, 2, 2)] + [Fake(96, 256, dtype=BF16)]
+    out = h.from_hidden(Fake(7, 96, dtype=BF16), *w, cu, pos, pos, stream=side)
+    assert out.stream is side and out.shape == (7, 96)
+    written = {name: args for name, args in calls.made}
+    assert {"mla_gqa_prompt_append", "mla_gqa_prompt_attn", "mla_gqa_prompt_out_proj", "mla_gqa_project"} <= set(written)
+
+
+def test_prompt_buffers_live_as_long_as_their_handle(calls, monkeypatch):
+    """Another width of hidden states does not give back what work still queued may be writing."""
+    h = handle(monkeypatch)
+    made, empty = [], torch.empty
+
+    def noted(*shape, **kw):
+        t = empty(*shape, **kw)
+        made.append(weakref.ref(t))
+        return t
+
+    monkeypatch.setattr(torch, "empty", noted)
+    cu, pos = Fake(3, dtype=I32), Fake(2, dtype=I32)
+    for hidden in (96, 128, 96, 128):
+        w = [Fake(n * 64, hidden, dtype=BF16) for n in (4, 2, 2)] + [Fake(hidden, 256, dtype=BF16)]
+        assert h.from_hidden(Fake(5, hidden, dtype=BF16), *w, cu, pos, pos).shape == (5, hidden)
+    assert len(made) == 5  # q, k, v; an output for either width
+    assert all(t() is not None for t in made)

@@ -32,3 +32,29 @@ def test_results_written_on_another_stream(raw):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(got_alpha, alpha)
     assert abi.check_status() == abi.MLA_OK
+
+
+def test_prompt_layers_on_another_stream():
+    """A handle's buffers of its first call, made while the current stream is busy with memory it has given up; hidden
+    states of another width; the current stream again."""
+    H, G, d, n = 8, 2, 64, [70, 40]
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    new = lambda *s: (torch.randn(*s, generator=gen, device="cuda") * s[-1] ** -0.5).bfloat16()  # noqa: E731
+    dims = abi.GqaDims(H, G, d, d ** -0.5)
+    cache = abi.Cache(*(torch.zeros(2 * G, 128, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)), 128)
+    cu, start, kv = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 70, 110], [0, 0], n))
+    work = [(new(110, D), *(new(m * d, D) for m in (H, G, G)), new(D, H * d)) for D in (512, 896)]
+    make = lambda: abi.GqaPrompt(dims, cache, 2, 110, 128)  # noqa: E731
+    want = [make().from_hidden(*w, cu, start, kv).clone() for w in work]
+    side, step = torch.cuda.Stream(), make()
+    torch.cuda.synchronize()
+    scratch = [torch.empty(110, m, dtype=torch.bfloat16, device="cuda") for m in (H * d, G * d, G * d, 512, 896) for _ in range(3)]
+    torch.cuda._sleep(20_000_000)
+    for s in scratch:
+        s.fill_(7)
+    del scratch, s
+    got = [step.from_hidden(*w, cu, start, kv, stream=side) for w in work + work[:1]]
+    torch.cuda.synchronize()
+    assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[0])
+    assert torch.equal(step.from_hidden(*work[1], cu, start, kv), want[1])
+    assert abi.check_status() == abi.MLA_OK
