@@ -461,7 +461,9 @@ mla_status mla_pages_fork(const mla_page_pool *pool, int32_t num_caches, const m
 /* Move the pages in use to the low end of the pool: with L pages in use, the
  * i-th used page at or above L moves to the i-th free page below L, in every
  * cache, and the whole table and the counts follow.  Afterwards pages L and up
- * are free (their old rows stay as they were). */
+ * are free (their old rows stay as they were).  A table entry whose page nothing
+ * counts is recorded as MLA_ERR_DEVICE_BOUNDS and left (its page may be one that
+ * another moves to). */
 mla_status mla_pages_compact(const mla_page_pool *pool, int32_t num_caches, const mla_cache *caches, int32_t c_width,
                              int32_t r_width, void *workspace, void *stream);
 

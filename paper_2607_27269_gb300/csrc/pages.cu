@@ -27,9 +27,9 @@ constexpr int kWorkThreads = 256, kCopyCtas = 6;
 constexpr int kChunk = 4 * kWorkThreads;  // vectors of a step of a compaction's copies
 constexpr int kHead = 16;  // ints before the workspace's lists
 
-// Workspace: [0] pages moved, [1] used pages; then a table row's copy each (source
+// Workspace: [0] pages moved; then a table row's copy each (source
 // page, page of its own or -1, rows); then one int a page each: free list or
-// destinations, sources, new places.
+// destinations, sources, new places (-1: nothing counts the page).
 struct Ws {
     int32_t *head;
     int4 *copy;
@@ -477,8 +477,8 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(mla_page_poo
             if (h >> plan.lane & 1) w.list[at.x + __popc(h & lower)] = page;
             if (m >> plan.lane & 1)
                 w.src[at.y + __popc(m & lower)] = page;
-            else if (page >= used && page < pages.y)
-                w.to[page] = -1;
+            else if (page < pages.y)
+                w.to[page] = look.free[j] >> plan.lane & 1 ? -1 : page;  // (nothing counts a free one)
             at.x += __popc(h);
             at.y += __popc(m);
         }
@@ -490,10 +490,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(mla_page_poo
         p.refs[dst] = p.refs[src];
         p.refs[src] = 0;
     }
-    if (plan.warp == 0 && plan.lane == 0) {
-        w.head[0] = total.y;
-        w.head[1] = used;
-    }
+    if (plan.warp == 0 && plan.lane == 0) w.head[0] = total.y;
 }
 
 // The table's entries, then the moved pages, 1024 vectors of a layer's page a step.
@@ -502,16 +499,16 @@ __global__ void __launch_bounds__(kWorkThreads, kCopyCtas) compact_kernel(mla_pa
 {
     griddep_wait();
     const Ws w(ws, p);
-    const int moves = w.head[0], used = w.head[1];
+    const int moves = w.head[0];
     const int64_t entries = static_cast<int64_t>(p.num_rows) * p.bt_stride;
     for (int64_t i = blockIdx.x * kWorkThreads + threadIdx.x; i < entries; i += gridDim.x * kWorkThreads) {
         const int page = p.block_table[i];
-        if (page < used && page >= -1) continue;
+        if (page == -1) continue;
         const int to = page >= 0 && page < p.num_pages ? w.to[page] : -1;
-        if (to >= 0)
-            p.block_table[i] = to;
-        else
+        if (to < 0)
             record_status(status, kStatusBounds);  // no such page, or one that nothing counts
+        else if (to != page)
+            p.block_table[i] = to;
     }
     const int vectors = p.page_size * ((c.width[0] + c.width[1]) / 8), chunks = (vectors + kChunk - 1) / kChunk;
     const int64_t jobs = static_cast<int64_t>(moves) * c.n * chunks;
