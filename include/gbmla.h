@@ -450,7 +450,8 @@ mla_status mla_pages_reserve(const mla_page_pool *pool, int32_t n, const int32_t
  * pages are shared (counts rise by one), the tokens of a partial last page are
  * copied to a free page of the child's own, in every cache.  A child holds no
  * pages before (an entry that does is recorded and left), and is nobody's
- * parent in the same call; a parent may have several children.
+ * parent in the same call; a parent may have several children.  A parent's page
+ * that nothing counts is recorded and not shared or copied.
  *   caches: host array of num_caches (1 .. 32) descriptors over this pool's
  *   pages (their block_table is not read); widths of their c_kv and k_rope rows
  *   in elements, multiples of 8 (the strides rule as everywhere). */

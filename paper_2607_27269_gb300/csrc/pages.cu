@@ -27,9 +27,10 @@ constexpr int kWorkThreads = 256, kCopyCtas = 6;
 constexpr int kChunk = 4 * kWorkThreads;  // vectors of a step of a compaction's copies
 constexpr int kHead = 16;  // ints before the workspace's lists
 
-// Workspace: [0] pages moved; then a table row's copy each (source
+// Workspace: [0] pages moved, [1] pages looked at; then a table row's copy each (source
 // page, page of its own or -1, rows); then one int a page each: free list or
-// destinations, sources, new places (-1: nothing counts the page).
+// destinations, sources, new places (-1: nothing counts the page)
+// or which pages were free, a bit each.
 struct Ws {
     int32_t *head;
     int4 *copy;
@@ -151,8 +152,10 @@ struct Look {
 
 // Ranks the warp's `mine` wanted pages among the cluster's and puts the lowest free
 // pages into list, as many as are wanted; the first rank, *found pages are there.
-// `look` has loaded the warp's first pages.
-__device__ __forceinline__ int rank_pages(const mla_page_pool &p, Plan &plan, Look &look, int mine, int32_t *list, int *found)
+// `look` has loaded the warp's first pages.  Where `bits` is given, which pages were
+// free is left there, a word for every 32 pages up to *looked.
+__device__ __forceinline__ int rank_pages(const mla_page_pool &p, Plan &plan, Look &look, int mine, int32_t *list, int *found,
+                                          int32_t *bits = nullptr, int32_t *looked = nullptr)
 {
     const int64_t round = int64_t{plan.warps} * kLook * 32;
     int at = 0, want = 0, have = 0;
@@ -169,8 +172,10 @@ __device__ __forceinline__ int rank_pages(const mla_page_pool &p, Plan &plan, Lo
             const int to = r + __popc(look.free[j] & ((1u << plan.lane) - 1u));
             if ((look.free[j] >> plan.lane & 1) && to < want) list[to] = static_cast<int>(page0) + 32 * j + plan.lane;
             r += __popc(look.free[j]);
+            if (bits && plan.lane == j && page0 + 32 * j < p.num_pages) bits[page0 / 32 + j] = static_cast<int32_t>(look.free[j]);
         }
         have += total.y;
+        if (bits && plan.warp == 0 && plan.lane == 0) *looked = static_cast<int>(min(p0 + round, int64_t{p.num_pages}));
     }
     plan.sync();  // the list is written
     *found = min(have, want);
@@ -316,46 +321,50 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(mla_page_pool p
     Look look;
     look.load(p, plan.first_look(), p.num_pages);
     const int2 units = plan.share(n * p.groups, 32);
-    // the unit's source page (-1: nothing to copy), and the entry that its own page goes to
-    auto source = [&](int i, int32_t **entry, int *rows, bool report) {
+    // The unit's source page: that of its partial last one (-1: nothing to copy, or a
+    // fault).  Asked before any page is given out, for a page that nothing counts may be.
+    auto source = [&](int i) {
         const int from = row_of(p, parents, i), to = row_of(p, children, i), len = lens[i / p.groups];
         if (from < 0 || to < 0 || from == to || !len_ok(p, len)) {
-            if (report) record_status(status, kStatusBounds);
+            record_status(status, kStatusBounds);
             return -1;
         }
-        *rows = len % p.page_size;
-        if (*rows == 0) return -1;
+        if (len % p.page_size == 0) return -1;
         const int k = len / p.page_size;
         const int src = p.block_table[static_cast<int64_t>(from) * p.bt_stride + k];
-        *entry = p.block_table + static_cast<int64_t>(to) * p.bt_stride + k;
-        const bool good = src >= 0 && src < p.num_pages && **entry == -1;
-        if (!good && report) record_status(status, kStatusBounds);
-        return good ? src : -1;
+        if (src >= 0 && src < p.num_pages && p.refs[src] > 0 && p.block_table[static_cast<int64_t>(to) * p.bt_stride + k] == -1)
+            return src;
+        record_status(status, kStatusBounds);
+        return -1;
     };
-    int mine = 0, rows;
-    int32_t *entry;
+    int mine = 0;
     for (int i0 = units.x; i0 < units.y; i0 += 32) {
         const int i = i0 + plan.lane;
-        mine += i < units.y && source(i, &entry, &rows, true) >= 0;
+        if (i >= units.y) break;
+        const int src = source(i);
+        w.copy[i].x = src;
+        mine += src >= 0;
     }
-    int found, at = rank_pages(p, plan, look, __reduce_add_sync(0xffffffffu, mine), w.list, &found);
+    __syncwarp();
+    int found, at = rank_pages(p, plan, look, __reduce_add_sync(0xffffffffu, mine), w.list, &found, w.to, &w.head[1]);
     for (int i0 = units.x; i0 < units.y; i0 += 32) {
         const int i = i0 + plan.lane;
-        const int src = i < units.y ? source(i, &entry, &rows, false) : -1;
+        const int src = i < units.y ? w.copy[i].x : -1;
         const unsigned who = __ballot_sync(0xffffffffu, src >= 0);
-        int page = -1;
+        int page = -1, rows = 0;
         if (src >= 0) {
-            const int r = at + __popc(who & ((1u << plan.lane) - 1u));
+            const int r = at + __popc(who & ((1u << plan.lane) - 1u)), len = lens[i / p.groups];
             if (r < found) {
                 page = __ldcg(w.list + r);
-                *entry = page;
+                rows = len % p.page_size;
+                p.block_table[static_cast<int64_t>(row_of(p, children, i)) * p.bt_stride + len / p.page_size] = page;
                 p.refs[page] = 1;
             } else {
                 record_status(status, kStatusBounds);
             }
         }
         at += __popc(who);
-        if (i < units.y) w.copy[i] = make_int4(src, page, page >= 0 ? rows : 0, 0);
+        if (i < units.y) w.copy[i] = make_int4(src, page, rows, 0);
     }
 }
 
@@ -407,12 +416,14 @@ __global__ void __launch_bounds__(kWorkThreads) fork_kernel(mla_page_pool p, con
     }
     const int from = row_of(p, parents, i), to = row_of(p, children, i), len = lens[i / p.groups];
     if (from < 0 || to < 0 || from == to || !len_ok(p, len)) return;
-    const int full = len / p.page_size;
+    const int full = len / p.page_size, looked = w.head[1];
     const int32_t *src = p.block_table + static_cast<int64_t>(from) * p.bt_stride;
     int32_t *dst = p.block_table + static_cast<int64_t>(to) * p.bt_stride;
     for (int k = threadIdx.x; k < full; k += kWorkThreads) {
         const int page = src[k];
-        if (page < 0 || page >= p.num_pages || dst[k] != -1) {
+        // (a page that nothing counts may have been given out since: what the plan saw tells)
+        if (page < 0 || page >= p.num_pages || dst[k] != -1 ||
+            (page < looked ? w.to[page / 32] >> (page % 32) & 1 : p.refs[page] <= 0)) {
             record_status(status, kStatusBounds);
             continue;
         }
