@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) logprobs_kernel(const Logprob
     constexpr int VN = Vec<T>::n, U = kUnroll;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int size = 1 << log_size, own = blockIdx.x & (size - 1), k = a.n_top;
-    griddep_launch_dependents();
     griddep_wait();
+    griddep_launch_dependents();
     const uint4 none = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
     // the CTA's i-th row: its own ones, then those of its cluster (there are less
     // than 2^31 rows, so that unsigned ones do not overflow)

@@ -456,8 +456,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tmem_alloc(smem_u32(&sh.tmem), 512);
         tc::tmem_relinquish();
     }
-    griddep_launch_dependents();
     griddep_wait();
+    griddep_launch_dependents();
     if (blockIdx.x == 0) {
         for (int b = tid; b < a.batch; b += kThreads) {
             const int kv = a.kv_len[b];
