@@ -519,6 +519,13 @@ mla_status mla_check_status(void *stream);
  * with mla_check_status(). */
 mla_status mla_selftest_wait_timeout(int64_t limit_ns, void *stream);
 
+/* The same of the bounded wait that counts its looks at the mbarrier instead of
+ * reading a clock (mla_gqa_prompt_attn's, 250000 looks): 1000 looks at one that
+ * nothing signals must run out and record MLA_ERR_DEVICE_TIMEOUT, and a phase
+ * that has ended must be seen (else MLA_ERR_DEVICE_BOUNDS is recorded too).  The
+ * looks' time in nanoseconds goes to *elapsed_ns (device, or NULL). */
+mla_status mla_selftest_wait_looks(int64_t *elapsed_ns, void *stream);
+
 /* Testing aid: re-read the GBMLA_* environment variables that choose the
  * kernels' tiling (they are otherwise read once per process, at the first
  * call that needs them): GBMLA_ATTN_KERNEL=simt (CUDA-core attention),

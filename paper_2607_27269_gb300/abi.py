@@ -26,6 +26,7 @@ EXPORTS = ("mla_workspace_size", "mla_cache_append", "mla_project_append", "mla_
            "mla_token_logprobs", "mla_pages_workspace_size", "mla_pages_release", "mla_pages_reserve",
            "mla_pages_fork", "mla_pages_compact", "mla_e2e_loss", "mla_absorb_q", "mla_decode_attn", "mla_combine",
            "mla_out_proj", "mla_decode_step", "mla_check_status", "mla_selftest_wait_timeout",
+           "mla_selftest_wait_looks",
            "mla_decode_attn_noalloc", "mla_reload_tuning", "mla_status_str", "mla_last_error")
 
 
@@ -116,6 +117,7 @@ def lib(auto_build: bool = True):
                                           i32, vp, vp, vp, vp, vp, vp, vp, vp]
             L.mla_check_status.argtypes = [vp]
             L.mla_selftest_wait_timeout.argtypes = [i64, vp]
+            L.mla_selftest_wait_looks.argtypes = [vp, vp]
             L.mla_decode_attn_noalloc.argtypes = [P(MlaDims), P(MlaCache), i32, i32, vp, i32, vp, i32, vp, vp, vp]
             L.mla_last_error.restype = ctypes.c_char_p
             L.mla_last_error.argtypes = []
@@ -668,6 +670,14 @@ def check_status(stream=None) -> int:
 
 def selftest_wait_timeout(limit_ns: int, stream=None):
     _check("mla_selftest_wait_timeout", lib().mla_selftest_wait_timeout(int(limit_ns), _stream(stream)))
+
+
+def selftest_wait_looks(elapsed_ns: Optional[torch.Tensor] = None, stream=None):
+    """1000 looks at an mbarrier that nothing signals (MLA_ERR_DEVICE_TIMEOUT afterwards); their time into the given
+    int64 device tensor."""
+    if elapsed_ns is not None and (elapsed_ns.dtype != torch.int64 or elapsed_ns.numel() < 1):
+        raise ValueError("elapsed_ns must be int64 and hold one entry")
+    _check("mla_selftest_wait_looks", lib().mla_selftest_wait_looks(_p(elapsed_ns), _stream(stream)))
 
 
 class DecodeStep:

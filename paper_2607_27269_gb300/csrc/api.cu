@@ -193,6 +193,8 @@ mla_status from_cuda(cudaError_t e)
     return MLA_ERR_CUDA;
 }
 
+constexpr int kSelftestLooks = 1000;
+
 __global__ void selftest_wait_kernel(uint64_t limit_ns, unsigned *status)
 {
     __shared__ __align__(8) uint64_t bar;
@@ -201,6 +203,28 @@ __global__ void selftest_wait_kernel(uint64_t limit_ns, unsigned *status)
     // Nothing arrives on `bar`: the bounded wait must give up.
     if (!mbar_wait(smem_u32(&bar), 0, limit_ns)) {
         if (threadIdx.x == 0) record_status(status, kStatusTimeout);
+    }
+}
+
+// The bounded wait that counts its looks (the prompt attention's): 1000 of them,
+// their time in nanoseconds; then a phase that has ended, which it must see.
+__global__ void selftest_looks_kernel(int64_t *elapsed_ns, unsigned *status)
+{
+    __shared__ __align__(8) uint64_t bar[2];
+    if (threadIdx.x == 0) {
+        mbar_init(&bar[0], 1);
+        mbar_init(&bar[1], 1);
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&bar[1])) : "memory");
+    }
+    __syncthreads();
+    const uint64_t t0 = global_ns();
+    const bool ran_out = !mbar_wait_looks<kSelftestLooks>(smem_u32(&bar[0]), 0);
+    const uint64_t t1 = global_ns();
+    const bool seen = mbar_wait_looks<kSelftestLooks>(smem_u32(&bar[1]), 0);
+    if (threadIdx.x == 0) {
+        if (ran_out) record_status(status, kStatusTimeout);
+        if (!seen) record_status(status, kStatusBounds);
+        if (elapsed_ns) *elapsed_ns = static_cast<int64_t>(t1 - t0);
     }
 }
 
@@ -221,6 +245,12 @@ void reload_tuning()
 cudaError_t launch_selftest_wait(int64_t limit_ns, unsigned *status, cudaStream_t st)
 {
     selftest_wait_kernel<<<1, 32, 0, st>>>(static_cast<uint64_t>(limit_ns), status);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_selftest_looks(int64_t *elapsed_ns, unsigned *status, cudaStream_t st)
+{
+    selftest_looks_kernel<<<1, 32, 0, st>>>(elapsed_ns, status);
     return cudaGetLastError();
 }
 
@@ -1051,6 +1081,15 @@ mla_status mla_selftest_wait_timeout(int64_t limit_ns, void *stream)
     mla_status s = device_info(&status, nullptr);
     if (s != MLA_OK) return s;
     return from_cuda(launch_selftest_wait(limit_ns, status, static_cast<cudaStream_t>(stream)));
+}
+
+mla_status mla_selftest_wait_looks(int64_t *elapsed_ns, void *stream)
+{
+    if (reinterpret_cast<uintptr_t>(elapsed_ns) % 8) return MLA_ERR_INVALID_ARG;
+    unsigned *status = nullptr;
+    const mla_status s = device_info(&status, nullptr);
+    if (s != MLA_OK) return s;
+    return from_cuda(launch_selftest_looks(elapsed_ns, status, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -87,6 +87,22 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, ui
     }
 }
 
+// The same without a clock: at most LOOKS looks, each of which sleeps until the
+// phase's end or for 3.8 us (as mla_selftest_wait_looks measures it).
+template <int LOOKS>
+__device__ __forceinline__ bool mbar_wait_looks(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, %3;\nLOOK_%=:\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n vote.sync.all.pred p, p, 0xffffffff;\n"
+        " sub.u32 n, n, 1;\n setp.ne.and.u32 q, n, 0, !p;\n @q bra LOOK_%=;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "n"(LOOKS)
+        : "memory");
+    return ok;
+}
+
 // ---------------------------------------------------------------- dependent launch
 // The kernels of a decode step are launched as programmatic dependents of
 // the previous launch: a kernel's prologue (barrier set-up, TMEM allocation,

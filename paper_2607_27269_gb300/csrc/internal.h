@@ -231,5 +231,6 @@ cudaError_t launch_e2e_loss(int rows, int hidden, const void *a_mla, const void 
                             float *loss, cudaStream_t st);
 
 cudaError_t launch_selftest_wait(int64_t limit_ns, unsigned *status, cudaStream_t st);
+cudaError_t launch_selftest_looks(int64_t *elapsed_ns, unsigned *status, cudaStream_t st);
 
 }  // namespace gbmla
