@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logprobs_kernel(const Logprob
         // ---- the pass: groups of vectors, the next group's loads ahead
         Run run{-INFINITY, kMasked, -INFINITY, -INFINITY, 0, 0, 0, 0};
         // the logits before the first vector (rank 0) and behind the last (the last rank)
-        const bool has_head = rank == 0 && tid < head, has_tail = rank == C - 1 && tail + tid < a.vocab;
+        const bool has_head = rank == 0 && tid < head, has_tail = rank == C - 1 && tid < a.vocab - tail;
         const uint4 ends[2] = {has_head ? Vec<T>::lone(x + tid) : none, has_tail ? Vec<T>::lone(x + tail + tid) : none};
         for (int at = 0; at < mine; at += 2 * U * kThreads) {
             if (at + U * kThreads < mine) at_row.fetch(v[1], at + U * kThreads);
