@@ -4,8 +4,9 @@
 // A row goes to one CTA or to a cluster of 2 or 4, each a slice of its vocabulary.
 // A thread keeps, over its vectors of 16 bytes, the maximum m and, over a base b
 // that follows it loosely, S = sum 2^((x - b) log2 e) and T = the same sum with
-// each term times its exponent; merged over the row,
-//     lse = m + ln S,  entropy = ln S - ln 2 T / S,  log p(y) = x_y - m - ln S.
+// each term times x - b (which is finite where its product with log2 e is not);
+// merged over the row,
+//     lse = m + ln S,  entropy = ln S - T / S,  log p(y) = x_y - m - ln S.
 // The alternatives need no second pass: the threads' maxima give a value that at
 // least n_top logits of the slice reach.  A thread knows its best groups of
 // vectors; those that reach that value are looked at again (a hundred of 4000) and
@@ -41,7 +42,7 @@ constexpr int kKeys = 4096;                 // keys put by in a slice
 constexpr int kGroups = 2048;               // groups of vectors that are looked at again
 constexpr int kRank = 512;                  // keys that are ranked one against the other
 constexpr int kPiece = 2048;                // logits of a piece, where those do not do
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMasked = -2e9f;            // logits at or below weigh nothing
 constexpr float kFloor = -1e30f;            // what lower ones are raised to: 2^-inf would be 0, but 0 x inf is not
 constexpr float kRaise = 16.f;              // a base is raised once a logit passes it by this much
@@ -174,7 +175,7 @@ struct Vec<uint16_t> {
 };
 
 // Statistics of some logits: the maximum, and over the base b the sums of 2^y and
-// of 2^y y, y = (x - b) log2 e.  (The difference first: x log2 e - b log2 e in one
+// of 2^y (x - b), y = (x - b) log2 e.  (The difference first: x log2 e - b log2 e in one
 // FMA saves an instruction a pair, but leaves the rounding of b log2 e in y, 64 for
 // logits of -1e9, and a lone token's probability is then not 1.)
 struct Stat {
@@ -183,7 +184,7 @@ struct Stat {
 // The same over another base.
 __device__ __forceinline__ void rebase(Stat &a, float b)
 {
-    const float d = (a.b - b) * kLog2e, f = ex2(d);
+    const float d = a.b - b, f = ex2(d * kLog2e);
     // (what weighs nothing any more may be large: no 0 x inf; but a sum that is NaN stays so)
     a.t = f > 0.f ? f * (a.t + d * a.s) : 0.f;
     a.s = f > 0.f ? f * a.s : a.s - a.s;
@@ -239,7 +240,7 @@ __device__ __forceinline__ void take(Run &r, const uint4 (&v)[N], int at)
     }
     r.m = fmaxf(r.m, m);
     if (r.m > r.b + kRaise) {
-        const float d = (r.b - r.m) * kLog2e, f = ex2(d);
+        const float d = r.b - r.m, f = ex2(d * kLog2e);
         float s0, s1, t0, t1;
         upk(r.s, s0, s1);
         upk(r.t, t0, t1);
@@ -256,12 +257,12 @@ __device__ __forceinline__ void take(Run &r, const uint4 (&v)[N], int at)
         Vec<T>::pairs(v[u], p);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const uint64_t x = mul2(add2(p[i], B), L);
+            const uint64_t d = add2(p[i], B);
             float a, b;
-            upk(x, a, b);
+            upk(mul2(d, L), a, b);
             const uint64_t e = pk(ex2(a), ex2(b));
             r.s = add2(r.s, e);
-            r.t = fma2(e, x, r.t);
+            r.t = fma2(e, d, r.t);
         }
     }
 }
@@ -591,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logprobs_kernel(const Logprob
             const float z = bad ? NAN : empty ? 0.f : logf(q.s);
             if (lane == 0) {
                 if (a.lse) a.lse[row] = empty ? -INFINITY : q.m + z;
-                if (a.entropy) a.entropy[row] = empty ? 0.f : z - q.t / q.s * kLn2;
+                if (a.entropy) a.entropy[row] = empty ? 0.f : z - q.t / q.s;
                 if (a.logprob && (token == -1 || (token >= 0 && token < a.vocab)))
                     a.logprob[row] = token == -1 ? 0.f
                                      : bad       ? NAN

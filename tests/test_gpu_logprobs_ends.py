@@ -11,6 +11,32 @@ from paper_2607_27269_gb300 import abi
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [9, 5000, 70000])
+def test_logits_as_large_as_the_type_holds(vocab, dtype):
+    """A token forced by a logit near the type's largest: probability 1, entropy 0, wherever it stands; two such tokens
+    share it."""
+    big = torch.finfo(dtype).max
+    places = [0, 1, vocab // 2, vocab - 1]
+    x = torch.randn(len(places) + 3, vocab, device="cuda").to(dtype)
+    for r, at in enumerate(places):
+        x[r, at] = big
+    x[4, 3] = x[4, vocab - 2] = big
+    x[5, 2] = 2.5e38
+    x[5, 5:] = torch.finfo(dtype).min
+    x[6, 4] = big
+    x[6, 5:] = -math.inf
+    t = torch.tensor(places + [3, 2, 4], dtype=torch.int32, device="cuda")
+    lse = torch.empty(7, device="cuda")
+    lp, ent, idx, top = abi.token_logprobs(x, t, 2, lse=lse)
+    assert abi.check_status() == abi.MLA_OK
+    # e^0 is exact, everything else underflows: ln 1 and ln 2 to a rounding
+    want = torch.tensor([0.0] * 4 + [math.log(2)] + [0.0] * 2, device="cuda")
+    assert ((ent - want).abs() <= 2.0 ** -21).all(), ent
+    assert ((lp + want).abs() <= 2.0 ** -21).all()
+    assert torch.equal(lse, x.gather(1, t.long()[:, None])[:, 0].float())
+    assert torch.equal(idx[:, 0], t) and idx[4].tolist() == [3, vocab - 2]
+
 
 @pytest.mark.parametrize("vocab,offset", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 1), (2 ** 31 - 100, 3)])
 def test_vocabularies_up_to_the_largest(vocab, offset):
