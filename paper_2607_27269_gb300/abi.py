@@ -7,7 +7,6 @@ library's kernels.  PyTorch supplies device memory and streams.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import threading
@@ -160,15 +159,18 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-_here = contextlib.nullcontext()
-
-
-def _memory_of(stream):
-    """Where what a call writes on ``stream`` is allocated: in that stream's memory, since a block of the current
-    stream's may still be in use by work queued there, and is handed out again there when its tensor goes."""
+def _new_on(stream):
+    """torch.empty for what a call writes on ``stream``: in that stream's memory, since a block of the current stream's
+    may still be in use by work queued there, and is handed out again there when its tensor goes."""
     if stream is None:
-        return _here
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+        return torch.empty
+    on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream))
+
+    def new(*shape, **kw):
+        with torch.cuda.stream(on):
+            return torch.empty(*shape, **kw)
+
+    return new
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -352,7 +354,9 @@ def _i32(t: Optional[torch.Tensor]):
 
 
 def _room(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, device: torch.device):
-    """A caller's tensor holds what a call writes: rows of `width` entries, one behind the other."""
+    """A caller's tensor holds what a call writes: rows of `width` entries (0: nothing), one behind the other."""
+    if width == 0:
+        return
     if t.dtype != dtype or t.device != device:
         raise ValueError(f"outputs must be {dtype} tensors on {device}")
     if t.numel() < rows * width or (t.dim() > 1 and t.shape[-1] != width) or not t.is_contiguous():
@@ -413,8 +417,7 @@ class GqaPrompt:
         H, G, w = d.num_heads, d.num_kv_groups, d.head_dim
         if q is not None and q_rot is None:
             if self._q is None:
-                with _memory_of(stream):
-                    self._q = torch.empty(self.max_tokens, H, w, dtype=torch.bfloat16, device=k.device)
+                self._q = _new_on(stream)(self.max_tokens, H, w, dtype=torch.bfloat16, device=k.device)
             q_rot = self._q[:total]
         _check("mla_gqa_prompt_append", lib().mla_gqa_prompt_append(
             *self._refs, batch, total, _i32(cu_seqlens), _i32(start_pos), *_rows(q, H, w, total),
@@ -444,8 +447,8 @@ class GqaPrompt:
         out [total, hidden] bf16."""
         d, (total, hidden) = self.dims, h.shape
         self._sizes(total, kv_len.shape[0])
-        with _memory_of(stream):
-            new = lambda *s: torch.empty(self.max_tokens, *s, dtype=torch.bfloat16, device=h.device)
+        if self._proj is None or hidden not in self._outs:
+            new = lambda *s: _new_on(stream)(self.max_tokens, *s, dtype=torch.bfloat16, device=h.device)
             if self._proj is None:
                 self._proj = (new(d.num_heads, d.head_dim), *(new(d.num_kv_groups, d.head_dim) for _ in range(2)))
             if hidden not in self._outs:
@@ -479,16 +482,19 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], n_top: 
     dev = logits.device
     if tokens is not None and (tokens.shape[0] != rows or tokens.device != dev):
         raise ValueError("tokens holds one entry per row, on the logits' device")
-    for t, width, dtype in ((logprob, 1, torch.float32), (entropy, 1, torch.float32), (lse, 1, torch.float32),
-                            (top_index, n_top, torch.int32), (top_logprob, n_top, torch.float32)):
-        if t is not None and width:
-            _room(t, rows, width, dtype, dev)
-    with _memory_of(stream):
-        if logprob is None and tokens is not None:
-            logprob = torch.empty(rows, dtype=torch.float32, device=dev)
-        entropy = torch.empty(rows, dtype=torch.float32, device=dev) if entropy is None else entropy
-        top_index = torch.empty(rows, n_top, dtype=torch.int32, device=dev) if top_index is None else top_index
-        top_logprob = torch.empty(rows, n_top, dtype=torch.float32, device=dev) if top_logprob is None else top_logprob
+    for t in (logprob, entropy, lse):
+        if t is not None:
+            _room(t, rows, 1, torch.float32, dev)
+    if top_index is not None:
+        _room(top_index, rows, n_top, torch.int32, dev)
+    if top_logprob is not None:
+        _room(top_logprob, rows, n_top, torch.float32, dev)
+    new = _new_on(stream)
+    if logprob is None and tokens is not None:
+        logprob = new(rows, dtype=torch.float32, device=dev)
+    entropy = new(rows, dtype=torch.float32, device=dev) if entropy is None else entropy
+    top_index = new(rows, n_top, dtype=torch.int32, device=dev) if top_index is None else top_index
+    top_logprob = new(rows, n_top, dtype=torch.float32, device=dev) if top_logprob is None else top_logprob
     _check("mla_token_logprobs", lib().mla_token_logprobs(
         rows, vocab, 0 if logits.dtype == torch.float32 else 1, logits.data_ptr(),
         logits.stride(0) if rows > 1 else vocab, _i32(tokens), n_top, _p(logprob), _p(entropy), _p(lse), _i32(top_index),
@@ -558,9 +564,7 @@ def e2e_loss(a_mla: torch.Tensor, a_orig: torch.Tensor, mask: Optional[torch.Ten
     post-W_O outputs, bf16 [.., D]); returns a one-element fp32 device tensor."""
     hidden = a_mla.shape[-1]
     rows = a_mla.numel() // hidden
-    if loss is None:
-        with _memory_of(stream):
-            loss = torch.empty(1, dtype=torch.float32, device=a_mla.device)
+    loss = _new_on(stream)(1, dtype=torch.float32, device=a_mla.device) if loss is None else loss
     _check("mla_e2e_loss", lib().mla_e2e_loss(rows, hidden, _p(a_mla), _p(a_orig), _p(mask), _p(loss),
                                               _stream(stream)))
     return loss
@@ -611,11 +615,11 @@ def acceptance_stats(draft: torch.Tensor, target: torch.Tensor, alpha: Optional[
         raise ValueError("logits must be CUDA tensors with unit inner stride and equal row strides")
     row_stride = draft.stride(0) if rows > 1 else vocab
     dev = draft.device
-    with _memory_of(stream):
-        alpha = torch.empty(rows, dtype=torch.float32, device=dev) if alpha is None else alpha
-        argmax_draft = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_draft is None else argmax_draft
-        argmax_target = torch.empty(rows, dtype=torch.int32, device=dev) if argmax_target is None else argmax_target
-        greedy = torch.empty(rows, dtype=torch.int32, device=dev) if greedy is None else greedy
+    new = _new_on(stream)
+    alpha = new(rows, dtype=torch.float32, device=dev) if alpha is None else alpha
+    argmax_draft = new(rows, dtype=torch.int32, device=dev) if argmax_draft is None else argmax_draft
+    argmax_target = new(rows, dtype=torch.int32, device=dev) if argmax_target is None else argmax_target
+    greedy = new(rows, dtype=torch.int32, device=dev) if greedy is None else greedy
     _check("mla_acceptance_stats", lib().mla_acceptance_stats(rows, vocab, 0 if draft.dtype == torch.float32 else 1,
                                                               draft.data_ptr(), target.data_ptr(), row_stride,
                                                               _p(alpha),
