@@ -377,7 +377,8 @@ class GqaPrompt:
     ``batch`` sequences and ``max_tokens`` tokens a call, with every buffer
     allocated once (the rotated queries', the projections' and each hidden
     width's at their first use, in the memory of that call's stream) and kept as
-    long as the handle, which has to outlive the work queued with it.  ``append`` writes a call's keys and values to the cache and
+    long as the handle, which has to outlive the work queued with it.  The cache's
+    tensors are those that it has at each call.  ``append`` writes a call's keys and values to the cache and
     rotates its queries, ``attend`` runs the causal attention over the cache
     (o [total, H, head_dim] bf16, ``lse`` [total, H]), ``__call__`` both, and
     ``from_hidden`` the whole layer from hidden states to its output
@@ -398,9 +399,22 @@ class GqaPrompt:
         self._outs = {}  # of from_hidden, by hidden width
         self._views = 0, self._o[:0], self._lse[:0]  # of the last call's length
         self.lse = self._views[2]
-        # the layer's descriptors are fixed: marshalled once
-        self._structs = (dims.c(), cache.c())
-        self._refs = tuple(ctypes.byref(s) for s in self._structs)
+        self._layer = self._marshalled()
+
+    def _marshalled(self):
+        """The layer's descriptors, and what of the cache they were made from."""
+        c = self.cache
+        structs = self.dims.c(), c.c()
+        return (*map(ctypes.byref, structs), c.c_kv, c.k_rope, c.block_table, c.capacity, c.num_pages, c.page_size, structs)
+
+    def _refs(self):
+        """The descriptors, made anew where the cache has changed."""
+        c = self.cache
+        dims, cache, c_kv, k_rope, table, capacity, pages, size, _ = self._layer
+        if (c.c_kv is not c_kv or c.k_rope is not k_rope or c.block_table is not table or c.capacity != capacity
+                or c.num_pages != pages or c.page_size != size):
+            self._layer = dims, cache, *_ = self._marshalled()
+        return dims, cache
 
     def _sizes(self, total: int, batch: int):
         if total > self.max_tokens or batch > self.batch:
@@ -420,7 +434,7 @@ class GqaPrompt:
                 self._q = _new_on(stream)(self.max_tokens, H, w, dtype=torch.bfloat16, device=k.device)
             q_rot = self._q[:total]
         _check("mla_gqa_prompt_append", lib().mla_gqa_prompt_append(
-            *self._refs, batch, total, _i32(cu_seqlens), _i32(start_pos), *_rows(q, H, w, total),
+            *self._refs(), batch, total, _i32(cu_seqlens), _i32(start_pos), *_rows(q, H, w, total),
             *_rows(k, G, w), *_rows(v, G, w, total), *_rows(q_rot, H, w, total), _stream(stream)))
         return q_rot
 
@@ -435,7 +449,7 @@ class GqaPrompt:
             self._views = total, self._o[:total], self._lse[:total]
         _, o, self.lse = self._views
         _check("mla_gqa_prompt_attn", lib().mla_gqa_prompt_attn(
-            *self._refs, batch, total, _i32(cu_seqlens), _i32(kv_len), self.max_kv_len, q, stride, self.num_splits,
+            *self._refs(), batch, total, _i32(cu_seqlens), _i32(kv_len), self.max_kv_len, q, stride, self.num_splits,
             *self._parts, o.data_ptr(), self.lse.data_ptr(), _stream(stream)))
         return o
 
@@ -507,28 +521,49 @@ class PagePool:
     block table: ``block_table`` [rows, entries] int32 (-1: no page; the tensor
     the caches carry), ``refs`` [pages] int32 (entries that hold a page; 0:
     free), ``groups`` table rows per sequence (G of the original GQA caches, 1
-    of the latent cache).  Sequences and lengths are int32 device tensors; all
+    of the latent cache).  All tensors are those that the pool and its
+    caches have at each call.  Sequences and lengths are int32 device tensors; all
     work is on the device, in stream order."""
 
     def __init__(self, caches, block_table: torch.Tensor, refs: torch.Tensor, groups: int = 1):
         self.caches, self.block_table, self.refs, self.groups = list(caches), block_table, refs, groups
-        if not self.caches or block_table.dim() != 2:
+        self._ws = []  # (the last one is in use; work on those before may still be queued)
+        self._marshal()
+
+    def _marshal(self):
+        """The descriptors of the pool and its caches, and what they were made from."""
+        table, refs = self.block_table, self.refs
+        if not self.caches or table.dim() != 2:
             raise ValueError("a pool has at least one cache and a 2-d block table")
         c = self.caches[0]
-        self._widths = c.c_kv.shape[2], c.k_rope.shape[2]
-        if any((x.c_kv.shape[2], x.k_rope.shape[2]) != self._widths for x in self.caches):
+        widths = c.c_kv.shape[2], c.k_rope.shape[2]
+        if any((x.c_kv.shape[2], x.k_rope.shape[2]) != widths for x in self.caches):
             raise ValueError("the caches of a pool have the same widths")
         if any(t.shape[0] < x.num_pages or t.shape[1] < x.page_size for x in self.caches for t in (x.c_kv, x.k_rope)):
             raise ValueError("a cache holds num_pages pages of page_size tokens")
-        self._c = MlaPagePool(refs.shape[0], c.page_size, groups, block_table.shape[0], block_table.shape[1],
-                              _i32(refs), _i32(block_table))
-        self._caches = (MlaCache * len(self.caches))(*(x.c() for x in self.caches))
+        self._c = MlaPagePool(refs.shape[0], c.page_size, self.groups, table.shape[0], table.shape[1], _i32(refs),
+                              _i32(table))
+        self._structs = (MlaCache * len(self.caches))(*(x.c() for x in self.caches))
         size = ctypes.c_size_t()
         _check("mla_pages_workspace_size", lib().mla_pages_workspace_size(ctypes.byref(self._c), ctypes.byref(size)))
-        self._ws = torch.empty(size.value // 4, dtype=torch.int32, device=refs.device)
-        # the pool's descriptors are fixed: marshalled once
-        self._ref, self._ws_p = ctypes.byref(self._c), self._ws.data_ptr()
-        self._cache_args = len(self.caches), self._caches, *self._widths
+        if not self._ws or self._ws[-1].numel() < size.value // 4:
+            self._ws.append(torch.empty(size.value // 4, dtype=torch.int32, device=refs.device))
+        self._ref, self._ws_p = ctypes.byref(self._c), self._ws[-1].data_ptr()
+        self._cache_args = len(self.caches), self._structs, *widths
+        self._of = table, refs, [t for x in self.caches for t in (x.c_kv, x.k_rope)]
+
+    def _pool(self):
+        """The pool's descriptor, made anew where its table or counts are other tensors."""
+        if self.block_table is not self._of[0] or self.refs is not self._of[1]:
+            self._marshal()
+        return self._ref
+
+    def _layers(self):
+        """The caches' descriptors, made anew where their tensors are others."""
+        now = [t for x in self.caches for t in (x.c_kv, x.k_rope)]
+        if len(now) != len(self._of[2]) or any(a is not b for a, b in zip(now, self._of[2])):
+            self._marshal()
+        return self._cache_args
 
     def _lists(self, first, *more):
         shape = first.shape
@@ -539,23 +574,24 @@ class PagePool:
 
     def release(self, sequences: torch.Tensor, lens: torch.Tensor, stream=None):
         """Give back the pages past the first lens[i] tokens of each sequence."""
-        _check("mla_pages_release", lib().mla_pages_release(self._ref, *self._lists(sequences, lens), _stream(stream)))
+        _check("mla_pages_release", lib().mla_pages_release(self._pool(), *self._lists(sequences, lens), _stream(stream)))
 
     def reserve(self, sequences: torch.Tensor, lens: torch.Tensor, stream=None):
         """Pages for the first lens[i] tokens of each sequence."""
-        _check("mla_pages_reserve", lib().mla_pages_reserve(self._ref, *self._lists(sequences, lens), self._ws_p,
+        _check("mla_pages_reserve", lib().mla_pages_reserve(self._pool(), *self._lists(sequences, lens), self._ws_p,
                                                             _stream(stream)))
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, lens: torch.Tensor, stream=None):
         """children[i] becomes a copy of the first lens[i] tokens of parents[i]: full pages shared, a partial last
         page copied."""
-        _check("mla_pages_fork", lib().mla_pages_fork(self._ref, *self._cache_args,
+        _check("mla_pages_fork", lib().mla_pages_fork(self._pool(), *self._layers(),
                                                       *self._lists(parents, children, lens), self._ws_p,
                                                       _stream(stream)))
 
     def compact(self, stream=None):
         """Move the pages in use to the low end of the pool."""
-        _check("mla_pages_compact", lib().mla_pages_compact(self._ref, *self._cache_args, self._ws_p, _stream(stream)))
+        _check("mla_pages_compact", lib().mla_pages_compact(self._pool(), *self._layers(), self._ws_p,
+                                                            _stream(stream)))
 
 
 def e2e_loss(a_mla: torch.Tensor, a_orig: torch.Tensor, mask: Optional[torch.Tensor] = None,
