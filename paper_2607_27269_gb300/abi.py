@@ -475,6 +475,12 @@ class GqaPrompt:
 
 def gqa_prompt_out_proj(dims: GqaDims, o: torch.Tensor, w_o: torch.Tensor, out: torch.Tensor, stream=None):
     """out [total, D] = W_O concat_h o (o bf16 [total, H, head_dim], as GqaPrompt gives it)."""
+    H, d = dims.num_heads, dims.head_dim
+    if o.dtype != torch.bfloat16 or tuple(o.shape[1:]) != (H, d):
+        raise ValueError(f"o must be bf16 [total, {H}, {d}]")
+    if w_o.dtype != torch.bfloat16 or w_o.dim() != 2 or w_o.shape[1] != H * d:
+        raise ValueError(f"w_o must be bf16 [hidden, {H * d}]")
+    _room(out, o.shape[0], w_o.shape[0], torch.bfloat16, o.device)
     _check("mla_gqa_prompt_out_proj", lib().mla_gqa_prompt_out_proj(ctypes.byref(dims.c()), o.shape[0], w_o.shape[0],
                                                                     _p(o), _p(w_o), _p(out), _stream(stream)))
     return out

@@ -178,3 +178,17 @@ def test_prompt_buffers_live_as_long_as_their_handle(calls, monkeypatch):
         assert h.from_hidden(Fake(5, hidden, dtype=BF16), *w, cu, pos, pos).shape == (5, hidden)
     assert len(made) == 5  # q, k, v; an output for either width
     assert all(t() is not None for t in made)
+
+
+def test_prompt_projection_operands_that_do_not_fit_are_refused(calls):
+    dims = abi.GqaDims(4, 2, 64, 0.125)
+    good = dict(o=Fake(7, 4, 64, dtype=BF16), w_o=Fake(96, 256, dtype=BF16), out=Fake(7, 96, dtype=BF16))
+    assert abi.gqa_prompt_out_proj(dims, **good) is good["out"]
+    assert abi.gqa_prompt_out_proj(dims, **{**good, "out": Fake(9, 96, dtype=BF16)}).shape == (9, 96)
+    for name, bad in (("o", Fake(7, 4, 64)),                                 # fp32, as the decode step's o is
+                      ("o", Fake(7, 4, 32, dtype=BF16)), ("o", Fake(7, 256, dtype=BF16)), ("out", Fake(6, 96, dtype=BF16)),
+                      ("out", Fake(7, 96)), ("out", Fake(7, 100, dtype=BF16)), ("w_o", Fake(96, 128, dtype=BF16)),
+                      ("w_o", Fake(96, 256))):
+        with pytest.raises(ValueError):
+            abi.gqa_prompt_out_proj(dims, **{**good, name: bad})
+    assert len(calls.made) == 2
