@@ -1,4 +1,4 @@
-"""Results and buffers of calls on streams other than the current one."""
+"""Results and buffers of calls on streams other than the current one, and calls on several streams at a time."""
 from __future__ import annotations
 
 import pytest
@@ -58,3 +58,35 @@ def test_prompt_layers_on_another_stream():
     assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[0])
     assert torch.equal(step.from_hidden(*work[1], cu, start, kv), want[1])
     assert abi.check_status() == abi.MLA_OK
+
+
+def test_two_pools_and_two_layers_at_a_time():
+    """Calls on two streams that nothing orders among one another: each pool ends as its own rules say, each handle's
+    results are those that it has alone."""
+    from tests.test_gpu_pages import Model
+    from tests.test_gpu_prompt import Layer, cu_of, i32
+
+    n, kv = [150, 3, 90], [4000, 60, 1500]
+    layers = [Layer(14, 2, 64, kv, True, seed=50 + i) for i in range(2)]
+    q = [L.normal(sum(n), 14, 64) for L in layers]
+    steps = [abi.GqaPrompt(L.dims, L.cache, 3, sum(n), 4000) for L in layers]
+    cu, lens = cu_of(n), i32(kv)
+    want = [(s.attend(x, cu, lens).clone(), s.lse.clone()) for s, x in zip(steps, q)]
+    pools = [Model(30, 2, 9, 500, (64, 64), 2, seed=52 + i) for i in range(2)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for turn in range(6):
+        for i, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                m = pools[i]
+                m.reserve([turn], [100 + 60 * turn + i])
+                m.fork([turn] * 3, [10 + 3 * turn, 11 + 3 * turn, 12 + 3 * turn], [100, 90 + 60 * turn, 64])
+                got[i] = steps[i].attend(q[i], cu, lens)
+                if turn % 2:
+                    m.release([turn - 1, 10 + 3 * turn], [0, 0])
+                    m.compact()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(got[i], want[i][0]) and torch.equal(steps[i].lse, want[i][1])
+        pools[i].check()
