@@ -367,7 +367,10 @@ mla_status mla_gqa_prompt_workspace_size(const mla_gqa_dims *dims, int32_t batch
  *   NULL; o_part / lse_part sized by mla_gqa_prompt_workspace_size (NULL where
  *   that gives 0).
  * fp32 sums and softmax; the weights are rounded to bf16 before they multiply
- * the values. */
+ * the values (the sum that they are divided by is that of the unrounded ones).
+ * Every run of the same call gives the same bits.  Where a row is cut follows
+ * the whole call's lengths and num_splits, so that its last bits may differ with
+ * the sequences beside it; with num_splits 1 nothing is cut and they do not. */
 mla_status mla_gqa_prompt_attn(const mla_gqa_dims *dims, const mla_cache *cache, int32_t batch, int32_t total,
                                const int32_t *cu_seqlens, const int32_t *kv_len, int32_t max_kv_len, const void *q_rot,
                                int64_t q_stride, int32_t num_splits, float *o_part, float *lse_part, void *o, float *lse,
@@ -398,7 +401,9 @@ mla_status mla_gqa_prompt_out_proj(const mla_gqa_dims *dims, int32_t total, int3
  *   other value outside [0, vocab) is recorded as MLA_ERR_DEVICE_BOUNDS);
  *   0 <= n_top <= 32.  Outputs, fp32 but for the indices (int32); any may be
  *   NULL: logprob, entropy, lse [rows], top_index, top_logprob [rows, n_top].
- * rows == 0: no-op.  All sums fp32 in a fixed order. */
+ * rows == 0: no-op.  All sums fp32, in an order that every run of the same call
+ * repeats.  The order follows the number of rows, the row's place among them and
+ * its alignment, so that a row's last bits may differ with the rows beside it. */
 mla_status mla_token_logprobs(int32_t rows, int32_t vocab, int32_t logits_dtype, const void *logits,
                               int64_t row_stride, const int32_t *tokens, int32_t n_top, float *logprob,
                               float *entropy, float *lse, int32_t *top_index, float *top_logprob, void *stream);

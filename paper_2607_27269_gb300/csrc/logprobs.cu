@@ -18,11 +18,11 @@
 // 640 rows took 105 us in place of 66.)
 //
 // Bound: memory, once the rows fill the SMs (912 rows of 128256 bf16 logits: 46 us
-// or 5.0 TB/s with 20 alternatives; 640 rows, which are 1.4 waves, 40 us with them
+// or 5.0 TB/s with 20 alternatives; 640 rows, which are 1.4 waves, 39 us with them
 // and 31 us without), then what a row costs in turn (reductions, barriers, the
 // ranking: 2 us of which the next row's first loads hide a part; the whole next row
 // prefetched into L2 meanwhile takes more from the rows under way: 912 rows 54 us).
-// A few rows are bound by that latency: 5.4 us for 3 rows of 32000.  Issue is next
+// A few rows are bound by that latency: 5.7 us for 3 rows of 32000.  Issue is next
 // (about five instructions a bf16 logit: unpacking, maximum, exponent, exponential
 // and two sums, two-wide where that exists).
 #include <math.h>

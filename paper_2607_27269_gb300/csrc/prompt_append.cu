@@ -4,7 +4,7 @@
 //
 // y = x cos(p theta_k) - x' sin(p theta_k) over head_dim / 2 pairs: three
 // operations a value against four bytes moved, so memory is the bound: 67584 tokens
-// of 32 + 2 x 8 heads of 64 into a paged cache, 830 MB, take 141 us, 5.9 TB/s.  A block
+// of 32 + 2 x 8 heads of 64 into a paged cache, 830 MB, take 133 us, 6.2 TB/s.  A block
 // takes up to eight tokens of all heads: the sine and cosine of a (token, pair)
 // are evaluated once, into shared memory, and serve every head; so are the
 // tokens' sequences, positions and pages.  Everything else moves in 16-byte

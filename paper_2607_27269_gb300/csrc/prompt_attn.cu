@@ -26,12 +26,14 @@
 //
 // Bound.  A half's tile costs the tensor pipe 525 cycles at D = 64 and 1025 at 128,
 // and the exponential units 512 (32 lanes a clock).  D = 128 comes close: 8191 tokens
-// of 24 heads in 270 us, 1.53 PFLOP/s, 2320 cycles a tile of both halves.  D = 64 is
-// bound by the chain of one half's softmax: wait, 128 scores out of TMEM (170 cycles),
+// of 24 heads in 272 to 279 us from box to box, 1.48 to 1.52 PFLOP/s, 2320 cycles a
+// tile of both halves.  D = 64 is bound by the chain of one half's softmax, with this
+// layout (128-key tiles, P beside S, two halves, whose warps store their own rows):
+// wait, 128 scores out of TMEM (170 cycles),
 // maximum (500), weights (950), store, hand over; 1930 cycles a tile of both halves,
 // the tensor pipe 53 % and the issue slots 57 % busy.  Chunks of 125 to 475 tokens
-// behind prefixes of 4000 to 16000 (14 heads, 2 groups) take 83 us, 32 prompts of 17
-// to 1009 tokens (32 heads, 8 groups) 89 us, where an item's ends (3400 cycles) weigh
+// behind prefixes of 4000 to 16000 (14 heads, 2 groups) take 84 us, 32 prompts of 17
+// to 1009 tokens (32 heads, 8 groups) 88 us, where an item's ends (3400 cycles) weigh
 // as much as two tiles.  Tried: twice the softmax warps, each half of a row's scores
 // (102 us for the chunks: the chain's waits double, its arithmetic does not halve);
 // no maximum after the first tile, a sum's overflow asking for another base instead
